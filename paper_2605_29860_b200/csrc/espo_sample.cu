@@ -686,8 +686,9 @@ __device__ __forceinline__ void sweep_dense(const Slice<T>& L, int begin, int en
         __syncwarp();
         const float first = queue[lane], second = queue[32 + lane];
         __syncwarp();
-        queue[lane] = second;
         waiting -= 32;
+        if (lane < waiting) queue[lane] = second;
+        __syncwarp();                // the next logit may be put there by another lane
         f(first, true);
       }
     }
