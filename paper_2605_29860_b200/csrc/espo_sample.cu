@@ -456,7 +456,7 @@ struct Shared {
   Order order;
   Crossing crossing;
   int32_t starts[kMaxChunks + 1];
-  int32_t max_id, picked;
+  int32_t max_id;         // lowest id found: of the largest logit, or by a draw from the sums
   int32_t bin_crossed, bin_clear;
   uint64_t scratch64[kWarps];
   uint32_t scratch32[kWarps];
@@ -1071,21 +1071,27 @@ __device__ __forceinline__ bool pick(const SampleArgs& A, const Row& R, const Ch
   __syncthreads();
   for (int w = 0; w < warp; ++w) before += sums[w];
   double at = before + upto - own;
+  // The borders between threads are rounded on either side for themselves, so the target may seem to lie in two threads'
+  // pieces: the lowest id is the token.
+  int mine = 0x7fffffff;
+  float mine_x = 0.0f;
   if (own > 0.0 && at <= target && target < before + upto) {
-    bool taken = false;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       const double w = R.weight(x[i]);
-      if (!taken && target < at + w && x[i] > -INFINITY) {
-        taken = true;
-        emit(A, R.r, p * kN + i, R.logp(x[i], R.z));
-        S.picked = 1;
+      if (mine == 0x7fffffff && target < at + w && x[i] > -INFINITY) {
+        mine = p * kN + i;
+        mine_x = x[i];
       }
       at += w;
     }
+    if (mine != 0x7fffffff) atomicMin(&S.max_id, mine);
   }
   __syncthreads();
-  return S.picked != 0;
+  const int token = S.max_id;
+  if (token == 0x7fffffff) return false;
+  if (mine == token) emit(A, R.r, token, R.logp(mine_x, R.z));
+  return true;
 }
 
 // The row's numbers from its chunks': a lane holds chunks lane and lane + 32, every warp alike.
@@ -1160,10 +1166,7 @@ __global__ void __launch_bounds__(kThreads, 4) row_kernel(const SampleArgs A) {
   const int in_batch = blockIdx.x, r = A.row0 + in_batch;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   __shared__ Shared S;
-  if (tid == 0) {
-    S.max_id = 0x7fffffff;
-    S.picked = 0;
-  }
+  if (tid == 0) S.max_id = 0x7fffffff;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   bool bad_slot;
