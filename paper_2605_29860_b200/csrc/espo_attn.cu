@@ -241,6 +241,7 @@ struct StageInfo {
 
 struct Queue {            // shared memory beside the stages
   uint64_t full[8], empty[8];
+  uint64_t meeting;       // of the computing warps
   StageInfo info[8];
   float2 ml[kComputeWarps][16];
   int abort_flag;
@@ -724,6 +725,7 @@ __global__ void __launch_bounds__(tile_threads(kColTiles), kColTiles == 1 ? 3 : 
       mbar_init(&Z.full[s], copying_warps(kColTiles));
       mbar_init(&Z.empty[s], kComputeWarps);
     }
+    mbar_init(&Z.meeting, kComputeWarps);
     Z.abort_flag = 0;
     mbar_init_fence();
   }
@@ -857,13 +859,14 @@ __global__ void __launch_bounds__(tile_threads(kColTiles), kColTiles == 1 ? 3 : 
   X.clear();
   const int q0 = kByQuery ? warp * 16 : 0;
   int stage = 0;
-  uint32_t parity = 0;
+  uint32_t parity = 0, meeting_parity = 0;
+  bool ok = true;
+  auto meet = [&]() { return ok = warps_meet(&Z.meeting, meeting_parity, abort_flag); };
   for (;;) {
-    if (!warp_wait(&Z.full[stage], parity, abort_flag)) {
-      *abort_flag = 1;
-      if (lane == 0 && A.status_out) atomicOr(A.status_out, ESPO_DEV_TIMEOUT);
-      break;       // no warp can be left at a barrier below: a tile that has arrived is seen by all four
-    }
+    // A warp whose wait runs out leaves the loop, although the tile may still come and be seen by the others: they meet
+    // bounded too, and leave at the next meeting.
+    ok = warp_wait(&Z.full[stage], parity, abort_flag);
+    if (!ok) break;
     const StageInfo I = Z.info[stage];
     if (I.flags & 4) break;
     const bool busy = q0 < A.per_kv;
@@ -878,7 +881,7 @@ __global__ void __launch_bounds__(tile_threads(kColTiles), kColTiles == 1 ? 3 : 
       if (I.valid != ~0ull) {            // each warp clears a quarter for all
         clear_values<kDim, kE4M3>(base + T::kMatrix, warp * 16, static_cast<uint32_t>(I.valid >> (16 * warp)) & 0xffffu);
         fence_proxy_async();             // the stage is the copies' again afterwards
-        asm volatile("bar.sync 2, 128;" ::: "memory");
+        if (!meet()) break;
       }
       if (busy) {
 #pragma unroll 1
@@ -912,7 +915,7 @@ __global__ void __launch_bounds__(tile_threads(kColTiles), kColTiles == 1 ? 3 : 
 #pragma unroll
         for (int i = 0; i < Acc::kQ; ++i) Z.ml[warp][X.query(i)] = make_float2(X.m[i], X.l[i]);
       }
-      asm volatile("bar.sync 2, 128;" ::: "memory");
+      if (!meet()) break;
       float keep[Acc::kQ];
 #pragma unroll
       for (int i = 0; i < Acc::kQ; ++i) {
@@ -950,11 +953,11 @@ __global__ void __launch_bounds__(tile_threads(kColTiles), kColTiles == 1 ? 3 : 
           }
       };
       if (warp >= 2) put();
-      asm volatile("bar.sync 2, 128;" ::: "memory");
+      if (!meet()) break;
       if (warp < 2) add(half);
-      asm volatile("bar.sync 2, 128;" ::: "memory");
+      if (!meet()) break;
       if (warp == 1) put();
-      asm volatile("bar.sync 2, 128;" ::: "memory");
+      if (!meet()) break;
       if (warp == 0) add(reinterpret_cast<float4*>(reduce) + 2 * kColTiles * kDim);
       mine = warp == 0;
     }
@@ -984,6 +987,10 @@ __global__ void __launch_bounds__(tile_threads(kColTiles), kColTiles == 1 ? 3 : 
         if (on[i]) dst[i][d] = __float2bfloat16(v * inv[i]);
       });
     }
+  }
+  if (!ok) {
+    *abort_flag = 1;
+    if (lane == 0 && A.status_out) atomicOr(A.status_out, ESPO_DEV_TIMEOUT);
   }
 }
 

@@ -128,6 +128,18 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volati
   return __all_sync(kFullMask, mbar_wait_bounded(bar, parity, abort_flag));
 }
 
+// The warps that `bar` counts meet: what each wrote before is seen by all after it.  False if one of them does not come; a warp
+// that has given up elsewhere raises the flag, so the others never wait for it at length (as they would at a barrier of the
+// block).  `parity` is the warp's own, 0 before the first meeting.
+__device__ __forceinline__ bool warps_meet(uint64_t* bar, uint32_t& parity, volatile int* abort_flag) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
+  // (a meeting that took place counts, however soon the flag was raised after it)
+  const bool ok = warp_wait(bar, parity, abort_flag) || __all_sync(kFullMask, mbar_try_wait(bar, parity));
+  parity ^= 1;
+  return ok;
+}
+
 // Last index i in [0, n) with off[i] <= x (off ascending, off[0] <= x): 32 probes a step, one per lane.
 __device__ __forceinline__ int warp_find(const int64_t* off, int n, int64_t x) {
   const int lane = threadIdx.x & 31;
