@@ -837,16 +837,18 @@ __global__ void __launch_bounds__(tile_threads(kColTiles), kColTiles == 1 ? 3 : 
       }
     }
     if (!ok) {
-      // a wait ran out: the copies in flight still write to this block's shared memory, so wait for them (bounded too)
       *abort_flag = 1;
       bad |= ESPO_DEV_TIMEOUT;
-      for (int i = 0; i < min(filled, kStages); ++i) {
-        if (--stage < 0) {
-          stage = kStages - 1;
-          parity ^= 1;
-        }
-        mbar_wait_bounded(&Z.full[stage], parity, nullptr);
+    }
+    // Copies in flight write to this block's shared memory, and the computing warps may give up before they arrive: the block
+    // lasts until they have (bounded too).  Without such a mishap the last tiles are waited for anyhow.  `stage` itself has
+    // been used up, unless the wait for it ran out.
+    for (int i = 0; i < min(filled, ok ? kStages - 1 : kStages); ++i) {
+      if (--stage < 0) {
+        stage = kStages - 1;
+        parity ^= 1;
       }
+      if (!warp_wait(&Z.full[stage], parity, nullptr)) bad |= ESPO_DEV_TIMEOUT;
     }
     bad = __reduce_or_sync(kFullMask, bad);
     if (bad && lane == 0 && A.status_out) atomicOr(A.status_out, bad);
