@@ -56,6 +56,7 @@ struct PrefixShared {
   uint64_t done;             // the item's products are complete
   uint64_t odd;              // the odd stream's maxima and sums are in place
   uint64_t written;          // the item's result has been read from tensor memory
+  uint64_t drained[2];       // the products of each issuing warp are complete, at the block's end
   uint64_t valid[8][2];      // by unit slot (e4m3: raw slot): a bit per token
   uint64_t tile_valid[8][2]; // the same for the softmax, by the block's running tile number: a tile's entry is written again
                              // with the eighth tile after it, whose key unit finds room only once this tile's product with
@@ -226,6 +227,15 @@ __device__ __forceinline__ void products_arrive(uint64_t* bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
 }
 
+// Waits (bounded) until everything the warp has issued is complete: nothing reads shared or tensor memory after that, whoever
+// gives up.  `bar` serves this one time.
+__device__ __forceinline__ bool products_end(uint64_t* bar) {
+  __syncwarp();
+  if (elect_one()) products_arrive(bar);
+  __syncwarp();
+  return warp_wait(bar, 0, nullptr);
+}
+
 // Byte offset of 16-byte chunk `chunk` (of eight numbers) of row `row` in a 128-row matrix of bf16.
 __device__ __forceinline__ uint32_t unit_offset(int row, int chunk) {
   return (chunk >> 3) * (128 * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
@@ -260,6 +270,8 @@ __global__ void __launch_bounds__(kPrefixThreads, 1)
     mbar_init(&Z.done, 1);
     mbar_init(&Z.odd, 4);
     mbar_init(&Z.written, 4);
+    mbar_init(&Z.drained[0], 1);
+    mbar_init(&Z.drained[1], 1);
     Z.abort_flag = 0;
     Z.factor = fmaxf(fabsf(A.to_log2), 1e-37f);      // not zero: a masked score has to stay -inf
     mbar_init_fence();
@@ -295,7 +307,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1)
     const CUtensorMap* map = keys ? &k_map : &v_map;
     const uint8_t* exps = keys ? A.cache.k_exp : A.cache.v_exp;
     int slot = 0, tile = 0;
-    uint32_t parity = 0, filled = 0, filled_parity = 0;            // filled: a bit per slot this warp has filled, and the phase
+    uint32_t parity = 0, filled = 0, filled_parity = 0;            // filled: a bit per slot this warp filled last, and the phase
     for (; ok && walk.next(A, I); tile += I.tiles) {
       const int32_t* table = A.seqs.prefix_pages + static_cast<int64_t>(__ldcg(A.work.seg_group + I.seg)) * A.seqs.max_prefix_pages;
       // Page ids four tiles at a time, lane 8 i + j for box j of the i-th, loaded four tiles before they are used.
@@ -311,6 +323,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1)
         // for every unit, the other warp's too: a phase passed over could be taken for the next of its parity
         if (2 * tile + p >= kSlots) ok = warp_wait(kE4M3 ? &Z.raw_free[slot] : &Z.free[slot], parity ^ 1, abort_flag);
         if (!ok) break;
+        filled &= ~(1u << slot);                                   // what was there is free
         if (is_key == keys) {
           if (t > 0 && (t & 3) == 0) {
             ids = next_ids;
@@ -361,9 +374,10 @@ __global__ void __launch_bounds__(kPrefixThreads, 1)
         }
       }
     }
-    if (!ok)        // a wait ran out: the copies in flight still write to this block's shared memory
-      for (int i = 0; i < kSlots; ++i)
-        if ((filled >> i) & 1u) mbar_wait_bounded(&Z.loaded[i], (filled_parity >> i) & 1u, nullptr);
+    // Copies in flight write to this block's shared memory, and another warp may give up before they arrive: the block lasts
+    // until they have (bounded too).
+    for (int i = 0; i < kSlots; ++i)
+      if ((filled >> i) & 1u) ok &= warp_wait(&Z.loaded[i], (filled_parity >> i) & 1u, nullptr);
     bad = __reduce_or_sync(kFullMask, bad);
   } else if (warp == 13) {
     // ---------------------------------------------------------------- scores: S = Q K^T
@@ -398,6 +412,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1)
       products[1] += I.tiles >> 1;
       item_parity ^= 1;
     }
+    ok &= products_end(&Z.drained[0]);
   } else if (warp == 14) {
     // ---------------------------------------------------------------- values: O += P V
     constexpr uint32_t kDesc = product_descriptor(kDim, true);
@@ -438,6 +453,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1)
       }
       item_parity ^= 1;
     }
+    ok &= products_end(&Z.drained[1]);
   } else if (warp >= 8) {
     // ---------------------------------------------------------------- queries, conversion, clearing
     const int r = (warp & 3) * 32 + lane;
