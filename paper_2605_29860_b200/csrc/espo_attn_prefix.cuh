@@ -46,8 +46,8 @@ struct PrefixShape {
 
 struct PrefixShared {
   uint64_t loaded[8];        // a copied unit (bf16) or raw unit (e4m3) has arrived
-  uint64_t free[8];          // the products have read a unit (bf16: and the clearing warps are past it)
-  uint64_t raw_free[4];      // e4m3: a raw unit has been converted
+  uint64_t free[8];          // the products have read a unit (bf16: and the clearing warps and the other copying warp are past it)
+  uint64_t raw_free[4];      // e4m3: a raw unit has been converted, and the copying warp that did not fill it is past it
   uint64_t ready[8];         // e4m3: a unit is converted; bf16: an incomplete value unit is cleared
   uint64_t scores[2];        // S of a stream's tile is complete
   uint64_t weights[2][2];    // P of a stream's half tile is written
@@ -257,10 +257,10 @@ __global__ void __launch_bounds__(kPrefixThreads, 1)
   if (tid == 0) {
     for (int i = 0; i < 8; ++i) {
       mbar_init(&Z.loaded[i], 1);
-      mbar_init(&Z.free[i], kE4M3 ? 1 : 5);
+      mbar_init(&Z.free[i], kE4M3 ? 1 : 6);
       mbar_init(&Z.ready[i], 4);
     }
-    for (int i = 0; i < 4; ++i) mbar_init(&Z.raw_free[i], 4);
+    for (int i = 0; i < 4; ++i) mbar_init(&Z.raw_free[i], 5);
     for (int i = 0; i < 2; ++i) mbar_init(&Z.scores[i], 1);
     for (int i = 0; i < 4; ++i) {
       mbar_init(&Z.weights[0][0] + i, 4);
@@ -367,6 +367,9 @@ __global__ void __launch_bounds__(kPrefixThreads, 1)
           }
           filled |= 1u << slot;
           filled_parity = (filled_parity & ~(1u << slot)) | (parity << slot);
+        } else if (lane == 0) {
+          // The slot is not free again before this warp has passed it: two phases on, the wait above would not know its own.
+          mbar_arrive(kE4M3 ? &Z.raw_free[slot] : &Z.free[slot]);
         }
         if (++slot == kSlots) {
           slot = 0;
