@@ -1025,7 +1025,7 @@ __global__ void __launch_bounds__(256) join_kernel(const AttnArgs A, const __gri
     const int64_t per = piece_length(total * A.cache.n_kv_heads, kPrefixBlocks, 1);
     const int in_seg = static_cast<int>(a) - __ldcg(W.seg_first + seg);
     const int tiles = (__ldcg(W.seg_len + seg) + kPrefixTile - 1) / kPrefixTile;
-    const int64_t x0 = head * total + __ldcg(W.seg_off + seg) + in_seg / A.rows_per_block * tiles;
+    const int64_t x0 = head * total + __ldcg(W.seg_off + seg) + tiles_before_row(in_seg, A.rows_per_block, tiles);
     p0 = quotient(x0, per);
     n_prefix = static_cast<int>(quotient(x0 + tiles - 1, per) - p0) + 1;
     in_block = in_seg % A.rows_per_block * A.per_kv + q;

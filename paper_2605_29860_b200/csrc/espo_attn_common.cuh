@@ -107,7 +107,7 @@ __device__ __forceinline__ void wait_for_previous_kernel() { asm volatile("gridd
 __device__ __forceinline__ void let_next_kernel_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // a / b for a >= 0, b > 0; the 64-bit division's hundred instructions only where they are needed.
-__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+__host__ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
   if (static_cast<uint64_t>(a | b) >> 32 == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
   return a / b;
 }
@@ -115,6 +115,19 @@ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
 // How many tiles of the line a block takes.
 __device__ __forceinline__ int64_t piece_length(int64_t line, int blocks, int least) {
   return max(quotient(line + blocks - 1, blocks), static_cast<int64_t>(least));
+}
+
+// A segment's part of the prefixes' line: query block after query block, each with every tile of the prefix.  In 64 bits: a
+// prefix of 2^29 tokens has 2^22 tiles, and 512 query blocks of it pass 31 bits.
+//
+// Tiles before the query block of the segment's row `row`.
+__host__ __device__ __forceinline__ int64_t tiles_before_row(int row, int rows_per_block, int tiles) {
+  return static_cast<int64_t>(row / rows_per_block) * tiles;
+}
+// The query block and the tile of the prefix that lie `at` tiles into the part.
+__host__ __device__ __forceinline__ void block_and_tile(int64_t at, int tiles, int& block, int& tile) {
+  block = static_cast<int>(quotient(at, tiles));
+  tile = static_cast<int>(at - static_cast<int64_t>(block) * tiles);
 }
 
 __device__ __forceinline__ void tma_2d(void* dst, const CUtensorMap* map, int x, int y, uint64_t* bar) {

@@ -103,11 +103,9 @@ struct PrefixWalk {
     }
     I.len = __ldcg(W.seg_len + seg);
     const int tiles = (I.len + kPrefixTile - 1) / kPrefixTile;
-    const int in_seg = static_cast<int>(x - head * total - __ldcg(W.seg_off + seg));
     I.head = head;
     I.seg = seg;
-    I.block = in_seg / tiles;
-    I.tile0 = in_seg - I.block * tiles;
+    block_and_tile(x - head * total - __ldcg(W.seg_off + seg), tiles, I.block, I.tile0);
     I.tiles = static_cast<int>(min(static_cast<int64_t>(tiles - I.tile0), x_end - x));
     I.first = __ldcg(W.seg_first + seg) + I.block * A.rows_per_block;
     I.rows = min(A.rows_per_block, __ldcg(W.seg_end + seg) - I.first);
