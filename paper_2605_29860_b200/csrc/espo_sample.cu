@@ -1148,13 +1148,26 @@ __device__ __forceinline__ Kind read_row(const SampleArgs& A, int in_batch, cons
   R.top_key = K::of(R.top);
   R.min_key = K::kLowest;
   if (P.min_p > 0.0f) {
-    // The smallest key whose weight reaches min_p lies within a unit or two of the rounded logarithm's: one probe a lane.
-    const float edge = fmaxf(static_cast<float>(static_cast<double>(R.top) + log(static_cast<double>(P.min_p)) * P.temperature),
-                             -3.38953139e38f);      // the lowest bf16
-    const uint32_t probe = max(K::of(edge), K::kLowest + 16u) - 16u + lane;
-    const bool enough = probe <= R.top_key && R.weight(K::value(probe)) >= static_cast<double>(P.min_p);
-    const unsigned ok = __ballot_sync(kFullMask, enough);
-    R.min_key = ok ? __shfl_sync(kFullMask, probe, __ffs(ok) - 1) : R.top_key;
+    // The smallest key whose logit lies at most -T ln(min_p) below the largest, sought from the lowest key to the largest
+    // logit's (which passes), 32 probes a step.  In 64 bits, and by the logits, not by their keys' distance from a rounded
+    // border: next to zero thousands of keys lie closer together than any rounding of it.
+    const double least = log(static_cast<double>(P.min_p)) * static_cast<double>(P.temperature);
+    uint32_t lo = K::kLowest, hi = R.top_key;
+    while (lo < hi) {
+      const uint32_t step = (hi - lo + 31) / 32;
+      const uint32_t probe = min(lo + lane * step, hi);
+      const bool enough = static_cast<double>(K::value(probe)) - static_cast<double>(R.top) >= least;
+      const unsigned ok = __ballot_sync(kFullMask, enough);
+      if (ok) {
+        const int first = __ffs(ok) - 1;
+        hi = __shfl_sync(kFullMask, probe, first);
+        if (first) lo += (first - 1) * step + 1;
+        else lo = hi;
+      } else {
+        lo += 31 * step + 1;
+      }
+    }
+    R.min_key = hi;
   }
   return kSampled;
 }
