@@ -339,6 +339,12 @@ struct RowQueries {
   float factor[2];
 };
 
+// The power of two 2^e that brings numbers of magnitude up to `top` into [2^14, 2^15), fp16's upper end: -113 for the largest
+// finite numbers, and for infinities, which stay what they are; at most 126, so that 2^-e is a normal number too.
+__device__ __forceinline__ int fp16_exponent(float top) {
+  return min(max(14 + 127 - static_cast<int>(__float_as_uint(top) >> 23), -113), 126);
+}
+
 template <int kDim, bool kE4M3>
 __device__ __forceinline__ void load_queries(RowQueries<kDim, kE4M3>& Q, const AttnArgs& A, int item, int head, int q0) {
   const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
@@ -377,7 +383,7 @@ __device__ __forceinline__ void load_queries(RowQueries<kDim, kE4M3>& Q, const A
       }
       top = fmaxf(top, __shfl_xor_sync(kFullMask, top, 1));
       top = fmaxf(top, __shfl_xor_sync(kFullMask, top, 2));
-      const int e = min(max(14 + 127 - static_cast<int>(__float_as_uint(top) >> 23), -100), 100);
+      const int e = fp16_exponent(top);
       const float up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
       Q.factor[r] *= __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
 #pragma unroll
@@ -387,11 +393,6 @@ __device__ __forceinline__ void load_queries(RowQueries<kDim, kE4M3>& Q, const A
       }
     }
   }
-}
-
-// Power of two 2^-e that brings numbers of magnitude up to `top` into [2^14, 2^15), fp16's upper end.
-__device__ __forceinline__ int fp16_exponent(float top) {
-  return min(max(14 + 127 - static_cast<int>(__float_as_uint(top) >> 23), -100), 100);
 }
 
 // Queries as the right operand, eight a tile; a lane's fragments belong to query lane/4 of each tile, its factors to the
