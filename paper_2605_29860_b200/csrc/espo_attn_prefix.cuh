@@ -62,7 +62,7 @@ struct PrefixShared {
                              // with the eighth tile after it, whose key unit finds room only once this tile's product with
                              // the values is complete
   float2 ml[128];
-  float factor;              // |scale| log2(e); its sign is in Q
+  float factor;              // |scale| log2(e), its sign is in Q; for a scale of zero Q is zero and this 1
   uint32_t tmem;
   int abort_flag;
 };
@@ -234,6 +234,9 @@ __device__ __forceinline__ bool products_end(uint64_t* bar) {
   return warp_wait(bar, 0, nullptr);
 }
 
+// Two bf16 numbers times zero: zeros, or NaN.
+__device__ __forceinline__ uint32_t times_zero(uint32_t w) { return pack_bf16x2(bf16_lo(w) * 0.0f, bf16_hi(w) * 0.0f); }
+
 // Byte offset of 16-byte chunk `chunk` (of eight numbers) of row `row` in a 128-row matrix of bf16.
 __device__ __forceinline__ uint32_t unit_offset(int row, int chunk) {
   return (chunk >> 3) * (128 * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
@@ -271,7 +274,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1)
     mbar_init(&Z.drained[0], 1);
     mbar_init(&Z.drained[1], 1);
     Z.abort_flag = 0;
-    Z.factor = fmaxf(fabsf(A.to_log2), 1e-37f);      // not zero: a masked score has to stay -inf
+    Z.factor = A.to_log2 != 0.0f ? fabsf(A.to_log2) : 1.0f;      // not zero: a masked score has to stay -inf
     mbar_init_fence();
   }
   __syncthreads();
@@ -462,7 +465,8 @@ __global__ void __launch_bounds__(kPrefixThreads, 1)
     uint32_t slot_parity = 0, raw_parity = 0, done_parity = 0;
     bool first_item = true;
     while (ok && walk.next(A, I)) {
-      // query r: head r % per_kv of the item's row r / per_kv; the sign of the scale goes here, exact
+      // query r: head r % per_kv of the item's row r / per_kv; the sign of the scale goes here, exact, and a scale of zero (an
+      // infinity times zero is NaN, as in the formula)
       if (!first_item) {
         ok = warp_wait(&Z.done, done_parity, abort_flag);      // the item before has used Q
         done_parity ^= 1;
@@ -483,6 +487,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1)
           v.y ^= flip;
           v.z ^= flip;
           v.w ^= flip;
+          if (A.to_log2 == 0.0f) v = make_uint4(times_zero(v.x), times_zero(v.y), times_zero(v.z), times_zero(v.w));
         }
         *reinterpret_cast<uint4*>(q_tile + unit_offset(r, c)) = v;
       }
