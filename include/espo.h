@@ -515,7 +515,7 @@ int espo_kv_gather(const espo_kv_cache* cache, const int32_t* cache_slots, int32
  *                  >= n_q_heads * head_dim), 16-byte aligned; out must not overlap q
  *   n_q_heads      a multiple of n_kv_heads, at most 64 per key/value head
  *   row_ids        device int32 [n_rows] or NULL (row i = slot i)
- *   scale          finite
+ *   scale          at most 2^127 in magnitude; q . k has to fit 32 bits as it stands, before the scale
  *   workspace      device, 256-byte aligned, at least espo_attention_workspace bytes; calls that share one must not
  *                  overlap on the device
  *   status_out     device uint32 or NULL: ESPO_DEV_BAD_SLOT, BAD_PAGE (page or group; the page's tokens, or the row's

@@ -1193,7 +1193,7 @@ int espo_attention(const espo_kv_cache* cache, const espo_sequences* seqs, const
   if (rc == ESPO_OK) rc = check_sequences(seqs);
   if (rc != ESPO_OK) return rc;
   if (!workspace || (n_rows > 0 && (!q || !out))) return ESPO_ERR_NULL;
-  if (!isfinite(scale)) return ESPO_ERR_BAD_PARAM;
+  if (!(fabsf(scale) <= 0x1p127f)) return ESPO_ERR_BAD_PARAM;      // NaN too; times log2(e) it has to stay finite
   const int64_t row = static_cast<int64_t>(n_q_heads) * cache->head_dim;
   if (q_stride < row || out_stride < row) return ESPO_ERR_BAD_SHAPE;
   if (q_stride % 8 || out_stride % 8 || !aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 256) ||

@@ -239,3 +239,11 @@ def test_structures_of_another_device_are_refused(monkeypatch):
                  lambda: espo.espo_kv_append(c, z, z, i, positions=i, rope=r)):
         with pytest.raises(ValueError, match="is on cuda:1, the current device is cuda:0"):
             call()
+
+
+def test_attention_scales_that_leave_32_bits_are_refused(lib):
+    """Scores are taken times log2(e) in 32 bits."""
+    for scale in (2.0 ** 127, -2.0 ** 127, 2.0 ** -149, 0.0):
+        assert attention(lib, n=0, q=None, out=None, scale=scale) == OK, scale
+    for scale in (1.8e38, -1.8e38, 3.4e38):
+        assert attention(lib, scale=scale) == PARAM, scale
