@@ -16,8 +16,9 @@ ESPO_ROPE_PLAIN, ESPO_ROPE_LINEAR, ESPO_ROPE_BY_PARTS = 0, 1, 2
 _CODES = {torch.float32: _b.ESPO_F32, torch.bfloat16: _b.ESPO_BF16}
 
 
-# (a decode step's calls take microseconds: the device is asked for without torch's lazy initialisation in between)
-_current_device = torch._C._cuda_getDevice
+# (a decode step's calls take microseconds: the device is asked for without torch's lazy initialisation in between; a torch
+# built without CUDA lacks that function, and the rest of the package works there)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _ptr(t: Optional[torch.Tensor], name: str, dtype, shape=None):

@@ -1,6 +1,9 @@
 """Refusals of the operators around the decode step, and the rotary frequency tables: all of it on the host (CPU only)."""
 import ctypes as C
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -247,3 +250,21 @@ def test_attention_scales_that_leave_32_bits_are_refused(lib):
         assert attention(lib, n=0, q=None, out=None, scale=scale) == OK, scale
     for scale in (1.8e38, -1.8e38, 3.4e38):
         assert attention(lib, scale=scale) == PARAM, scale
+
+
+def test_the_package_imports_where_torch_has_no_cuda():
+    """A torch built without CUDA lacks its private device functions; the sharding helpers and generators work there."""
+    code = """
+import torch
+for name in [n for n in dir(torch._C) if n.startswith("_cuda_")]:
+    delattr(torch._C, name)
+import paper_2605_29860_b200 as espo
+from paper_2605_29860_b200 import shard, synth
+try:
+    espo.espo_kv_cache(*[torch.zeros(2, 1, 16, 64, dtype=torch.bfloat16)] * 2)
+except ValueError as e:
+    print(e)
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(espo.__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True)
+    assert r.returncode == 0 and "must be a CUDA tensor" in r.stdout, r.stderr
