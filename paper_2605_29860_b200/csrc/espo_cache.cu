@@ -130,14 +130,16 @@ __device__ __forceinline__ void from_pairs(Unit& u, bool adjacent) {
   u.b = make_float4(m.a.z, m.b.z, m.a.w, m.b.w);
 }
 
-// Cosine and sine of position * inv_freq, times mscale.  The product and its reduction to a part of a turn are 64-bit: at
-// position 10^6 a 32-bit product would be off by 0.06 rad.
+// Cosine and sine of position * inv_freq, times mscale, in 64 bits and rounded once.  The product and its reduction to a part
+// of a turn need 64 bits (at position 10^6 a 32-bit product would be off by 0.06 rad).  The functions take them for the entries
+// next to a border between two codes: with 32-bit ones 1709 of 41 million bf16 keys were rounded to the other side (20000 fp32
+// tokens, four batches), now 763, which the 32-bit rotation leaves; 8191 tokens to e4m3 take 41.5 us with their read-back, not 40.5.
 __device__ __forceinline__ void angle_of(int position, double inv_freq, float mscale, float& c, float& s) {
   const double turns = static_cast<double>(position) * inv_freq * 0.15915494309189533577;   // 1 / (2 pi)
-  const float part = static_cast<float>(turns - rint(turns));                                // in [-1/2, 1/2]
-  sincospif(2.0f * part, &s, &c);
-  c *= mscale;
-  s *= mscale;
+  double sine, cosine;
+  sincospi(2.0 * (turns - rint(turns)), &sine, &cosine);                                     // of at most half a turn
+  c = static_cast<float>(cosine * static_cast<double>(mscale));
+  s = static_cast<float>(sine * static_cast<double>(mscale));
 }
 
 constexpr int kAppendWarps = 8;
