@@ -84,8 +84,8 @@ extern "C" {
                                   /* espo_reset_state before the state is used again)      */
 #define ESPO_DEV_NAN_VALUE   8u   /* a value estimate was NaN (that row did not stop)       */
 #define ESPO_DEV_BAD_LENGTHS 16u  /* espo_advantages: sum(lengths) != total_tokens or L < 0 */
-                                  /* espo_attention, espo_kv_append_rows: a length outside   */
-                                  /* [0, max_pages * page_size], clamped                     */
+                                  /* espo_attention: a length outside [0, max_pages *        */
+                                  /* page_size], clamped; espo_kv_append_rows: not written   */
 #define ESPO_DEV_BAD_PAGE    32u  /* a page, cache slot or group outside the cache or tables; its tokens are left out */
 #define ESPO_DEV_CACHE_FULL  64u  /* espo_kv_append_rows: a row's pages are full, its token was not written          */
 
@@ -472,7 +472,8 @@ int espo_rope_frequencies(int32_t kind, double theta, int32_t rot_dim, double fa
  *   key, value     device [n_tokens, n_kv_heads, head_dim], dtype ESPO_F32 or ESPO_BF16, tokens key_stride /
  *                  value_stride ELEMENTS apart (slices of a fused projection)
  *   cache_slots    device int32 [n_tokens]: where each token goes; a negative entry skips the token's cache write
- *                  (its query is still rotated); entries must be distinct, else one of the tokens is kept
+ *                  (its query is still rotated); the others must be distinct: what a slot that is named twice
+ *                  holds afterwards is unspecified, and may be parts of both tokens
  *   positions      device int32 [n_tokens]; needed with rope
  *   rope           host pointer or NULL (no rotation; positions unused)
  *   q, q_out       device [n_tokens, n_q_heads, head_dim] of the same dtype, or both NULL with n_q_heads 0; q_out may
@@ -515,7 +516,7 @@ int espo_kv_gather(const espo_kv_cache* cache, const int32_t* cache_slots, int32
  *                  >= n_q_heads * head_dim), 16-byte aligned; out must not overlap q
  *   n_q_heads      a multiple of n_kv_heads, at most 64 per key/value head
  *   row_ids        device int32 [n_rows] or NULL (row i = slot i)
- *   scale          at most 2^127 in magnitude; q . k has to fit 32 bits as it stands, before the scale
+ *   scale          at most 2^127 in magnitude; q . k itself, before the scale, has to be finite as a 32-bit float
  *   workspace      device, 256-byte aligned, at least espo_attention_workspace bytes; calls that share one must not
  *                  overlap on the device
  *   status_out     device uint32 or NULL: ESPO_DEV_BAD_SLOT, BAD_PAGE (page or group; the page's tokens, or the row's
@@ -535,8 +536,10 @@ int espo_attention(const espo_kv_cache* cache, const espo_sequences* seqs, const
 int espo_attention_workspace(const espo_kv_cache* cache, int32_t n_rows, int32_t n_q_heads, int64_t* bytes_out);
 
 /* One token per row from given random numbers, every row with its own sampling parameters (the request's, where
- * espo_step has one set per rollout batch and draws its own noise).  With w_a = exp((x_a - max x) / T), Z their sum, and
- * A(a), n(a) the mass and the number of ids strictly more probable than a, the support is
+ * espo_step has one set per rollout batch and draws its own noise).  It stands in place of espo_step's draw, not before it:
+ * the step scores the token that it draws itself, so a rollout that early stopping watches takes its tokens from the step, and
+ * this call serves rows without it (evaluation, requests with parameters of their own).  With w_a = exp((x_a - max x) / T),
+ * Z their sum, and A(a), n(a) the mass and the number of ids strictly more probable than a, the support is
  *   { a : x_a > -inf,  A(a) < top_p Z,  n(a) < top_k,  w_a >= min_p }
  * (the rule of espo_params.top_p / top_k, so equally probable ids stay or go together), and the token is the lowest
  * supported id whose running sum of supported weights, in id order, exceeds u times their total.
@@ -557,7 +560,8 @@ int espo_attention_workspace(const espo_kv_cache* cache, int32_t n_rows, int32_t
  *                  temperature negative, above 1e30 or NaN): token 0, logp NaN;
  *                  ESPO_DEV_BAD_SLOT for a slot outside [0, capacity): token -1; ESPO_DEV_TIMEOUT if a bounded wait
  *                  ran out (that row: token 0, logp NaN)
- * Weights and their sums are 64-bit (exponential: relative error below 2^-38); inside a support found by a filter they are
+ * Weights and their sums are 64-bit (exponential: relative error below 2^-38; min_p compares x_a - max x with T ln min_p
+ * instead); inside a support found by a filter they are
  * rounded to multiples of 2^-42 of the largest one and added up as integers, so that the token does not depend on the order
  * of the additions; an id whose weight is below 2^-43 of the largest is not drawn there.
  * V at most 2^19.  Enqueued on `stream`.  Errors: NULL, BAD_DTYPE, BAD_SHAPE, ALIGN, CAPACITY (V,
