@@ -6,7 +6,8 @@
 // There m runs over t_j + e_j, so that the folded weight 2^(t_j + e_j - m) is at most 1 however far the values' sizes are
 // apart, while the plain weight 2^(t_j - m) that l adds up is at most 2^64.  As fp16 the folded weight is taken 2^15 times
 // larger (o too, until the end): weights down to 2^-29 of the largest keep all bits, and the rounding step never exceeds
-// 2^-39 of it.
+// 2^-39 of it.  Against a bf16 cache the weights are bf16 (off by 2^-8 of each at most), the type of the values in the same
+// instruction.  The sum l takes the weights before either rounding.
 //
 // What bounds it: a row's own tokens are read once for the few query heads of one key/value head (7 heads: 7 multiply-adds a
 // byte of bf16), far below the tensor cores' ratio, so those are bound by HBM; a prefix is read once for the query heads of

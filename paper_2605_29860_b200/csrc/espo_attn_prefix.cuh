@@ -7,13 +7,18 @@
 // weights over in halves of 64 tokens.  A maximum is only moved when a score exceeds it by more than 8 doublings, which is
 // rare after the first tiles: until then weights are at most 2^8, and O need not be read back and rescaled.
 //
+// Roundings.  The weights become bf16 for the product with the values (at most 2^-8 of each; the sum l takes them unrounded), since
+// one instruction's operands share a type, and the values are bf16: a cache's own, or e4m3 codes with exponents that no other 16-bit
+// type holds.  For an e4m3 prefix fp16 weights would be eight times finer; they need the values' exponents folded into them.
+//
 // What bounds it: a stream's chain of product, softmax (1200 clocks a half: loading scores 300, maximum 100, exponentials
 // 740) and product, 4100 clocks for a tile of each of the two streams, against 1024 a tile for the exponentials alone (16 a
 // clock and SM) and 768 for the products.  e4m3 pages add the conversion (by instruction to half
 // and float, on to bf16): about 2700 clocks a tile; moving the codes' bits into place instead took 3700, on the integer pipe that
 // the softmax needs too (8 groups of 32, 64 dims: 67 us, now 54).  Before an item's first product lie about 8 us: the plan, the walk to the item, its queries.
-// One group of 64 rows, 28 query heads on 4 of 128 dims, 40000 tokens of bf16: 59 us, 580 TFLOP/s, tensor
-// pipe 31 % active; 64 groups of 8 with up to 700 tokens, bf16: 25 us.  Measured and dropped: one
+// One group of 64 rows, 28 query heads on 4 of 128 dims, 40000 tokens of bf16: 60 us, 580 TFLOP/s, tensor
+// pipe 31 % active; 64 groups of 8 with up to 700 tokens: bf16 24 us, e4m3 42.  All 128 registers that 512 threads leave each are
+// taken, with 28 bytes spilled.  Measured and dropped: one
 // warp for both operands' copies (79 us: 1750 clocks to issue a unit), products of 64 keys (62), a second set of four
 // converting warps with 96 registers a thread (while codes were still moved by bits: 64 groups of 8 on e4m3 pages 241 us against
 // 237, 64-dim heads 137 against 141).

@@ -18,9 +18,12 @@
 //
 // What bounds it: HBM, one read of the logits; for 64-bit sums the 64-bit pipe (13 operations an id, 64 a clock and SM), which
 // is why ids are only summed where a sum is needed; issue slots are scarcer still (39 an id, 72 % taken), so a logit becomes a
-// double by the conversion instruction, not by four integer ones (200 x 151669 fp32: 58.0 -> 54.6 us).  512 rows of 152064 bf16 ids: 64 us with top_k alone, 108 without a filter;
-// mixed filters 97 us in the first kernel (64-bit pipe 41 % active, issuing 65 %), 15 in the second, 57 in the third; 512 wide
-// supports 600 us.
+// double by the conversion instruction, not by four integer ones (200 x 151669 fp32: 58.0 -> 53.7 us).  With top_k or min_p alone
+// nothing is summed in 64 bits, and a block's own chain bounds it (one load of its chunk, the search for its cut, two to four
+// barriers, the list, the listed logits read again), the other three blocks of its SM being all that hides it.  512 rows of
+// 152064 bf16 ids: 64 us with top_k alone, 62 with min_p, 101 without a filter, the mode 32; mixed filters 92 us in the first
+// kernel (64-bit pipe 43 % active, issuing 62 %), 15 in the second, 58 in the third, which its sweeps' latency bounds (issuing
+// 11 %; at 64 registers a thread it spills 378 bytes); 512 wide supports 730 us.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -44,10 +47,10 @@ constexpr int kMaxChunks = 64;              // of 8192 fp32 or 16384 bf16 ids
 constexpr int kListTotal = 2048;            // ids that all chunks' lists of a row hold together
 constexpr int kPerThread = 4;               // listed ids per thread when a floor is sought
 constexpr int kListed = kThreads * kPerThread;
-constexpr int kCluster = 8;                 // with four, some 120 wide rows of 152064 ids took 104 us, not 57; 512 take the same
+constexpr int kCluster = 8;                 // with four, some 120 wide rows of 152064 ids took 104 us, not 57, and 512 of them 579, not 730
 constexpr int kClusters = 74;               // of the third kernel: four blocks on every SM
 constexpr int kParts = kCluster * kWarps / 32;      // of the cluster's warps, per lane of one
-constexpr int kMaxRows = 2048;              // rows per pair of launches: what the workspace is sized for
+constexpr int kMaxRows = 2048;              // rows per three launches: what the workspace is sized for
 constexpr int kNear = 128;                  // keys a warp keeps of a bracket
 constexpr int kBins = 1024;
 constexpr float kBinsPerUnit = 32.0f;       // bins per doubling of the weight
